@@ -370,12 +370,17 @@ typedef struct {
 } realb_linear_io;
 int realb_linear_fp8(const realb_linear_io* io, void* stream);
 
-/* The gated feed-forward block: G,U = x . w13^T, h = silu(G)*U in FP32, encoded to E4M3 in blocks of 128 along I,
- * out = h . w2^T (+ add), BF16.  H and I multiples of 128.  w13 [2I, H]: rows [0,I) gate, [I,2I) up; w2 [H, I].
+/* The gated feed-forward block: G,U = x . w13^T, h = silu(G)*U, encoded to E4M3 in blocks of 128 along I,
+ * out = h . w2^T (+ add), BF16.  Sums: of up to 64 rows, and with REALB_SUMS_F32, FP32 throughout.  Otherwise both products take the 8-bit matrix
+ * instruction with the cut described at realb_linear_fp8, which here does not disappear in the output's rounding: about one code of h in 1000 falls
+ * on the other side of a rounding boundary, and out is typically 0.0018 to 0.0026 (few rows and columns: up to 0.0039) off the formula, relative
+ * in the norm, where FP32 sums leave 0.0017.  A row's bits then change where a batch grows past 64 rows.  H and I multiples of 128.  w13 [2I, H]: rows [0,I) gate, [I,2I) up; w2 [H, I].
  * workspace: realb_gated_ffn_workspace_bytes(T, I) bytes that start at a multiple of 16; its contents need not outlive the call (of more than 64
  * rows h stays there: codes [T, I], then scales [I/128, T rounded up to 4]). */
+enum { REALB_SUMS_MFMA8 = 0, REALB_SUMS_F32 = 1 };
 typedef struct {
     int T, H, I;
+    int sums;                                    /* REALB_SUMS_* */
     const uint8_t* x_q; long long ld_x; const float* x_s; long long ld_xs;
     const uint8_t* w13_q; const float* w13_s; const uint8_t* w2_q; const float* w2_s;
     const void* add; long long ld_add;           /* bf16 [T,H] or NULL; may be out itself */

@@ -11,11 +11,10 @@
 // it (found with single products, whatever the tile); the sums of 8 add up in FP32.  On blocks of normal values its sums are 1.5e-5
 // of their rms off, with one channel in 64 twenty times as large 5e-5.  Against the rounding of a BF16 output (1.7e-3) that is
 // nothing; h of the feed-forward block gets codes on the other side of a rounding boundary about once in 1000, and its output is 0.0018 to 0.0026
-// off the formula (small calls up to 0.0039) where FP32 sums leave 0.0017.  Gate/up on the BF16 instruction would avoid that, for half
-// the speed (3001 rows, H 2048, I 768 30.7 -> 46.5 us; 65 rows, I 1408 22 -> 31 us): not taken beyond 64 rows.  FP32 outputs are for
-// callers who want FP32 sums: there the codes are widened to BF16, which holds every E4M3 number, and multiplied by
-// v_mfma_f32_16x16x32_bf16 (1e-8), at half the rate.  Up to 64 rows that costs nothing, the weights' bytes being what takes the time,
-// so all calls of so few rows do it.
+// off the formula (small calls up to 0.0039) where FP32 sums leave 0.0017.  Callers who want FP32 sums ask for them, by FP32 outputs or
+// by REALB_SUMS_F32: there the codes are widened to BF16, which holds every E4M3 number, and multiplied by v_mfma_f32_16x16x32_bf16 (1e-8), at half
+// the rate and in the smaller tiles.  The feed-forward block, 8-bit instruction / FP32 sums: 65 rows, H 2048, I 1408 21.6 / 33.0 us; 3001 rows, I 768 30.9 / 54.5;
+// 65 536 rows, I 1408 529 / 1177.  Up to 64 rows that costs nothing, the weights' bytes being what takes the time, so all calls of so few rows do it.
 #include "fp8_device.h"
 #include "ffn_device.h"
 #include <climits>
@@ -226,7 +225,8 @@ struct SmallGeo {
     static_assert(TA % 64 == 0 && (TA + TW) % (8 * WAVES) == 0, "tile shapes");
 };
 
-template <bool GATEUP, bool F32OUT, int RT, int WM, int WN, int NS, int CT>
+// WIDE: FP32 sums, on the BF16 instruction.
+template <bool GATEUP, bool WIDE, bool F32OUT, int RT, int WM, int WN, int NS, int CT>
 __global__ void __launch_bounds__(64 * WM * WN) fp8_tile_kernel(const Fp8Gemm p) {
     using G = SmallGeo<RT, WM, WN, NS, CT>;
     constexpr int TA = G::TA, OPS = G::OPS, COLS = GATEUP ? G::TW / 2 : G::TW;
@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(64 * WM * WN) fp8_tile_kernel(const Fp8Gemm p)
         for (int i = 0; i < RT; ++i) {                     // the transfers go out between the MFMAs: a wave blocks while one is accepted
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < CT; ++t) fp8_mma<F32OUT>(acc[i][t], fw[t], fx[i], xs[i] * (t < 2 ? s0 : s1));
+            for (int t = 0; t < CT; ++t) fp8_mma<WIDE>(acc[i][t], fw[t], fx[i], xs[i] * (t < 2 ? s0 : s1));
             __builtin_amdgcn_sched_barrier(0);
             if (kb + NS - 1 < p.KB) issue(i * EACH, min((i + 1) * EACH, OPS + 1), kb + NS - 1, smem + fill * G::STAGE);
         }
@@ -689,7 +689,7 @@ __global__ void __launch_bounds__(64 * WAVES) fp8_few_kernel(const Fp8Gemm p) {
 
 static int current_device(int* dev) { REALB_HIP(hipGetDevice(dev)); return REALB_OK; }
 
-template <bool GATEUP, bool F32OUT, int RT, int WM, int WN, int NS, int CT>
+template <bool GATEUP, bool WIDE, bool F32OUT, int RT, int WM, int WN, int NS, int CT>
 static int launch_fp8_small(Fp8Gemm p, hipStream_t s) {
     using G = SmallGeo<RT, WM, WN, NS, CT>;
     static_assert(G::LDS <= 160 * 1024, "LDS");
@@ -698,7 +698,7 @@ static int launch_fp8_small(Fp8Gemm p, hipStream_t s) {
     const int rc = current_device(&dev);
     if (rc != REALB_OK) return rc;
     if (first_use_on_device(seen, dev)) {
-        REALB_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_tile_kernel<GATEUP, F32OUT, RT, WM, WN, NS, CT>), hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS));
+        REALB_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_tile_kernel<GATEUP, WIDE, F32OUT, RT, WM, WN, NS, CT>), hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS));
         mark_used_on_device(seen, dev);
     }
     const int rows = ceil_div(p.M, G::TA), cols = ceil_div(p.N, GATEUP ? G::TW / 2 : G::TW);
@@ -709,7 +709,7 @@ static int launch_fp8_small(Fp8Gemm p, hipStream_t s) {
     p.rows_first = p.M < (GATEUP ? 2 : 1) * p.N;
     p.panel_tiles = p.rows_first ? rows : cols;
     division_magic(p.panel_tiles, &p.panel_magic, &p.panel_shift);
-    hipLaunchKernelGGL((fp8_tile_kernel<GATEUP, F32OUT, RT, WM, WN, NS, CT>), dim3((unsigned)(8 * ((tiles + 7) / 8))), dim3(64 * G::WAVES), G::LDS, s, p);
+    hipLaunchKernelGGL((fp8_tile_kernel<GATEUP, WIDE, F32OUT, RT, WM, WN, NS, CT>), dim3((unsigned)(8 * ((tiles + 7) / 8))), dim3(64 * G::WAVES), G::LDS, s, p);
     REALB_HIP(hipGetLastError());
     return REALB_OK;
 }
@@ -764,19 +764,22 @@ static int launch_fp8_few(const Fp8Gemm& p, hipStream_t s) {
 }
 // Which tiles: those with the least time by rounds of them on the chip.  A round's time at K = 2048, us, where a round is one tile on every
 // slot, that is as many blocks as run at once:
-//                              BF16 out  F32 out (half the rate)
+//                              8-bit     FP32 sums (half the rate)
 //   64 x 64                        9       12    a block per CU
 //   128 x 64                      11       17    a block per CU
 //   128 x 128, 16 waves           15       26    a block per CU, one round
 //   128 x 128, 8 or 4 waves       21       40    two blocks per CU
 //   256 x 256                     25
-//   gate/up, h columns half the weight rows, a block per CU: 64 x 256 15;  128 x 256 22;  256 x 256 31
+//   gate/up, h columns half the weight rows, a block per CU:
+//   64 x 256                      15       24
+//   128 x 256                     22       37
+//   256 x 256                     31
 // Where the last round of 256-row tiles would be short, the rows behind the whole rounds go to a second launch with smaller tiles, if that is
 // faster by more than a launch: 10 000 rows, K = N = 2048 51.2 -> 48.5 us; the feed-forward block of 6000 rows, H 2048, I 1408 82.7 -> 71.7 us.
 enum Fp8Tile { kTile64, kTile128x64, kTile128One, kTile128, kTile256, kTileSplit };      // (Split: whole rounds of 256 and a second launch)
 struct Fp8Choice { Fp8Tile tile; int us; };
 
-template <bool GATEUP, bool F32OUT>
+template <bool GATEUP, bool WIDE>
 static Fp8Choice choose_tiles(const Fp8Gemm& p, int M, int cus, int* whole) {
     auto rounds = [&](int rows, int cols, int per_cu) {
         const long long slots = (long long)per_cu * cus;
@@ -786,56 +789,61 @@ static Fp8Choice choose_tiles(const Fp8Gemm& p, int M, int cus, int* whole) {
     auto offer = [&](Fp8Tile tile, int us) { if (us < best.us) best = Fp8Choice{tile, us}; };
     const int one = GATEUP ? 31 : 25;                      // a round of 256-row tiles
     const int cols = GATEUP ? 128 : 256;                   // their output columns
-    if (!F32OUT && p.KB <= kBigMaxBlocks && p.ld_x <= kBigMaxPitch) {
+    if (!WIDE && p.KB <= kBigMaxBlocks && p.ld_x <= kBigMaxPitch) {
         offer(kTile256, one * rounds(256, cols, 1));
         const int wide = ceil_div(p.N, cols);
         const long long full = (long long)ceil_div(M, 256) * wide / cus, rows = full * cus / wide * 256;      // whole rounds, rows of them
         if (whole && full > 0 && rows > 0 && rows < M) {
             constexpr int kLaunch = 3;
             *whole = (int)rows;
-            offer(kTileSplit, (int)full * one + kLaunch + choose_tiles<GATEUP, F32OUT>(p, M - (int)rows, cus, nullptr).us);
+            offer(kTileSplit, (int)full * one + kLaunch + choose_tiles<GATEUP, WIDE>(p, M - (int)rows, cus, nullptr).us);
         }
     }
     if (GATEUP) {
-        offer(kTile128, 22 * rounds(128, 128, 1));
-        offer(kTile64, 15 * rounds(64, 128, 1));
+        offer(kTile128, (WIDE ? 37 : 22) * rounds(128, 128, 1));
+        offer(kTile64, (WIDE ? 24 : 15) * rounds(64, 128, 1));
     } else {
-        offer(kTile128, (F32OUT ? 40 : 21) * rounds(128, 128, 2));
-        if (rounds(128, 128, 1) == 1) offer(kTile128One, F32OUT ? 26 : 15);
-        offer(kTile128x64, (F32OUT ? 17 : 11) * rounds(128, 64, 1));
-        offer(kTile64, (F32OUT ? 12 : 9) * rounds(64, 64, 1));
+        offer(kTile128, (WIDE ? 40 : 21) * rounds(128, 128, 2));
+        if (rounds(128, 128, 1) == 1) offer(kTile128One, WIDE ? 26 : 15);
+        offer(kTile128x64, (WIDE ? 17 : 11) * rounds(128, 64, 1));
+        offer(kTile64, (WIDE ? 12 : 9) * rounds(64, 64, 1));
     }
     return best;
 }
 
-template <bool GATEUP, bool F32OUT>
+template <bool GATEUP, bool WIDE, bool F32OUT>
 static int launch_fp8_tiles_of(const Fp8Gemm& p, Fp8Tile tile, bool stream, hipStream_t s) {
     if constexpr (GATEUP) {
-        if (tile == kTile256) return launch_fp8_big<true, false, false>(p, s);
-        if (tile == kTile128) return launch_fp8_small<true, false, 2, 4, 4, 3, 4>(p, s);
-        return launch_fp8_small<true, false, 2, 2, 4, 3, 4>(p, s);
+        if constexpr (WIDE) {                               // (widened codes of 16 waves a block would not fit the registers)
+            if (tile == kTile128) return launch_fp8_small<true, true, false, 4, 2, 4, 3, 4>(p, s);
+        } else {
+            if (tile == kTile256) return launch_fp8_big<true, false, false>(p, s);
+            if (tile == kTile128) return launch_fp8_small<true, false, false, 2, 4, 4, 3, 4>(p, s);
+        }
+        return launch_fp8_small<true, WIDE, false, 2, 2, 4, 3, 4>(p, s);
     } else {
-        if constexpr (F32OUT) {
-            if (tile == kTile128) return launch_fp8_small<false, true, 4, 2, 2, 2, 4>(p, s);
+        if constexpr (WIDE) {
+            if (tile == kTile128) return launch_fp8_small<false, true, F32OUT, 4, 2, 2, 2, 4>(p, s);
         } else {
             if (tile == kTile256 && p.K % 128 != 0) return stream ? launch_fp8_big<false, true, true>(p, s) : launch_fp8_big<false, true, false>(p, s);
             if (tile == kTile256) return stream ? launch_fp8_big<false, false, true>(p, s) : launch_fp8_big<false, false, false>(p, s);
-            if (tile == kTile128) return launch_fp8_small<false, false, 2, 4, 2, 2, 4>(p, s);
+            if (tile == kTile128) return launch_fp8_small<false, false, false, 2, 4, 2, 2, 4>(p, s);
         }
-        if (tile == kTile128One) return launch_fp8_small<false, F32OUT, 2, 4, 4, 4, 2>(p, s);
-        return tile == kTile64 ? launch_fp8_small<false, F32OUT, 1, 4, 2, 4, 2>(p, s) : launch_fp8_small<false, F32OUT, 2, 4, 2, 4, 2>(p, s);
+        if (tile == kTile128One) return launch_fp8_small<false, WIDE, F32OUT, 2, 4, 4, 4, 2>(p, s);
+        return tile == kTile64 ? launch_fp8_small<false, WIDE, F32OUT, 1, 4, 2, 4, 2>(p, s) : launch_fp8_small<false, WIDE, F32OUT, 2, 4, 2, 4, 2>(p, s);
     }
 }
 
-template <bool GATEUP, bool F32OUT>
+template <bool GATEUP, bool WIDE, bool F32OUT>
 static int launch_fp8_tile(const Fp8Gemm& p, hipStream_t s) {
+    static_assert(WIDE || !F32OUT, "F32 outputs have FP32 sums");
     int cus = 0;
     int rc = static_scratch_lookup(nullptr, &cus);
     if (rc != REALB_OK) return rc;
     int whole = 0;
-    const Fp8Choice c = choose_tiles<GATEUP, F32OUT>(p, p.M, cus, &whole);
+    const Fp8Choice c = choose_tiles<GATEUP, WIDE>(p, p.M, cus, &whole);
     const bool stream = !GATEUP && (long long)p.M * p.N * 2 > kStreamBytes;
-    if (c.tile != kTileSplit) return launch_fp8_tiles_of<GATEUP, F32OUT>(p, c.tile, stream, s);
+    if (c.tile != kTileSplit) return launch_fp8_tiles_of<GATEUP, WIDE, F32OUT>(p, c.tile, stream, s);
     Fp8Gemm head = p, rest = p;
     head.M = whole;
     rest.M = p.M - whole;
@@ -844,9 +852,9 @@ static int launch_fp8_tile(const Fp8Gemm& p, hipStream_t s) {
     rest.out += whole * p.ld_out * (GATEUP ? 1 : F32OUT ? 4 : 2);
     if (GATEUP) rest.out_s += whole;
     if (p.add) rest.add += whole * p.ld_add * (F32OUT ? 4 : 2);
-    rc = launch_fp8_tiles_of<GATEUP, F32OUT>(head, kTile256, stream, s);
+    rc = launch_fp8_tiles_of<GATEUP, WIDE, F32OUT>(head, kTile256, stream, s);
     if (rc != REALB_OK) return rc;
-    return launch_fp8_tiles_of<GATEUP, F32OUT>(rest, choose_tiles<GATEUP, F32OUT>(rest, rest.M, cus, nullptr).tile, stream, s);
+    return launch_fp8_tiles_of<GATEUP, WIDE, F32OUT>(rest, choose_tiles<GATEUP, WIDE>(rest, rest.M, cus, nullptr).tile, stream, s);
 }
 
 static int check_rows(const uint8_t* q, long long ld, const float* s, long long ld_s, long long rows, int K) {
@@ -880,7 +888,7 @@ int realb_linear_fp8(const realb_linear_io* io, void* stream) {
     p.ld_x = io->ld_x; p.ld_xs = io->ld_xs; p.ld_out = io->ld_out; p.ld_add = io->ld_add;
     p.M = io->M; p.N = io->N; p.K = io->K; p.KB = ceil_div(io->K, 128);
     if (p.M <= kFewRows) return f32 ? launch_fp8_few<kFewLinearF32>(p, as_stream(stream)) : launch_fp8_few<kFewLinear>(p, as_stream(stream));
-    return f32 ? launch_fp8_tile<false, true>(p, as_stream(stream)) : launch_fp8_tile<false, false>(p, as_stream(stream));
+    return f32 ? launch_fp8_tile<false, true, true>(p, as_stream(stream)) : launch_fp8_tile<false, false, false>(p, as_stream(stream));
 }
 
 size_t realb_gated_ffn_workspace_bytes(int T, int I) {
@@ -897,6 +905,7 @@ int realb_gated_ffn_fp8(const realb_ffn_io* io, void* stream) {
     REALB_REQUIRE(io != nullptr, REALB_EINVAL, "io is NULL");
     REALB_REQUIRE(io->T >= 0 && io->H > 0 && io->I > 0 && io->H % 128 == 0 && io->I % 128 == 0 && io->H <= 65536 && io->I <= 65536, REALB_ESHAPE,
                   "T=%d H=%d I=%d: H and I must be positive multiples of 128 up to 65536", io->T, io->H, io->I);
+    REALB_REQUIRE(io->sums == REALB_SUMS_MFMA8 || io->sums == REALB_SUMS_F32, REALB_EINVAL, "bad choice of sums %d", io->sums);
     if (io->T == 0) return REALB_OK;
     REALB_REQUIRE(io->x_q && io->x_s && io->w13_q && io->w13_s && io->w2_q && io->w2_s && io->out && io->workspace, REALB_EINVAL, "NULL argument");
     const int rc = check_rows(io->x_q, io->ld_x, io->x_s, io->ld_xs, io->T, io->H);
@@ -923,8 +932,12 @@ int realb_gated_ffn_fp8(const realb_ffn_io* io, void* stream) {
         const int rc1 = launch_fp8_few<kFewGateUp>(a, s);
         return rc1 != REALB_OK ? rc1 : launch_fp8_few<kFewDown>(b, s);
     }
-    const int rc1 = launch_fp8_tile<true, false>(a, s);
-    return rc1 != REALB_OK ? rc1 : launch_fp8_tile<false, false>(b, s);
+    if (io->sums == REALB_SUMS_F32) {
+        const int rc1 = launch_fp8_tile<true, true, false>(a, s);
+        return rc1 != REALB_OK ? rc1 : launch_fp8_tile<false, true, false>(b, s);
+    }
+    const int rc1 = launch_fp8_tile<true, false, false>(a, s);
+    return rc1 != REALB_OK ? rc1 : launch_fp8_tile<false, false, false>(b, s);
 }
 
 }  // extern "C"
