@@ -863,6 +863,13 @@ static int check_rows(const uint8_t* q, long long ld, const float* s, long long 
     return REALB_OK;
 }
 
+// What h of T rows takes.
+static size_t ffn_h_bytes(int T, int I) {
+    if (T <= kFewRows) return (size_t)T * I * 4;            // FP32
+    const size_t pitch = ((size_t)T + 3) / 4 * 4;
+    return (size_t)T * I + pitch * (I / 128) * 4;          // codes and scales
+}
+
 }  // namespace realb
 
 using namespace realb;
@@ -896,9 +903,8 @@ size_t realb_gated_ffn_workspace_bytes(int T, int I) {
         set_error("T=%d I=%d: I must be a positive multiple of 128", T, I);
         return 0;
     }
-    if (T <= kFewRows) return (size_t)T * I * 4;            // h in FP32
-    const size_t pitch = ((size_t)T + 3) / 4 * 4;
-    return (size_t)T * I + pitch * (I / 128) * 4;          // codes and scales
+    const size_t need = ffn_h_bytes(T, I), few = ffn_h_bytes(kFewRows, I);
+    return T > kFewRows && need < few ? few : need;         // (a workspace for T rows holds any smaller batch)
 }
 
 int realb_gated_ffn_fp8(const realb_ffn_io* io, void* stream) {
@@ -912,8 +918,8 @@ int realb_gated_ffn_fp8(const realb_ffn_io* io, void* stream) {
     if (rc != REALB_OK) return rc;
     REALB_REQUIRE(aligned_to(io->w13_q, 16) && aligned_to(io->w2_q, 16) && aligned_to(io->w13_s, 4) && aligned_to(io->w2_s, 4) && aligned_to(io->workspace, 16), REALB_EINVAL,
                   "codes and workspace must start at multiples of 16 bytes");
-    REALB_REQUIRE(io->workspace_bytes >= realb_gated_ffn_workspace_bytes(io->T, io->I), REALB_EINVAL, "the workspace has %zu bytes, T=%d I=%d needs %zu",
-                  io->workspace_bytes, io->T, io->I, realb_gated_ffn_workspace_bytes(io->T, io->I));
+    REALB_REQUIRE(io->workspace_bytes >= ffn_h_bytes(io->T, io->I), REALB_EINVAL, "the workspace has %zu bytes, T=%d I=%d needs %zu",
+                  io->workspace_bytes, io->T, io->I, ffn_h_bytes(io->T, io->I));
     REALB_REQUIRE(io->ld_out >= io->H && aligned_to(io->out, 2), REALB_EINVAL, "rows of out must be H=%d apart or more", io->H);
     REALB_REQUIRE(!io->add || (io->ld_add >= io->H && aligned_to(io->add, 2)), REALB_EINVAL, "rows of add must be H=%d apart or more", io->H);
     hipStream_t s = as_stream(stream);
