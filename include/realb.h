@@ -376,7 +376,7 @@ int realb_linear_fp8(const realb_linear_io* io, void* stream);
  * on the other side of a rounding boundary, and out is typically 0.0018 to 0.0026 (few rows and columns: up to 0.0039) off the formula, relative
  * in the norm, where FP32 sums leave 0.0017.  A row's bits then change where a batch grows past 64 rows.  H and I multiples of 128.  w13 [2I, H]: rows [0,I) gate, [I,2I) up; w2 [H, I].
  * workspace: realb_gated_ffn_workspace_bytes(T, I) bytes that start at a multiple of 16, enough for calls of fewer rows too; its contents need not
- * outlive the call (of more than 64 rows h stays there: codes [T, I], then scales [I/128, T rounded up to 4]). */
+ * outlive the call, and it serves one call at a time (of more than 64 rows h stays there: codes [T, I], then scales [I/128, T rounded up to 4]). */
 enum { REALB_SUMS_MFMA8 = 0, REALB_SUMS_F32 = 1 };
 typedef struct {
     int T, H, I;

@@ -69,6 +69,7 @@ class FfnIO(C.Structure):
                 ("w13_q", C.c_void_p), ("w13_s", C.c_void_p), ("w2_q", C.c_void_p), ("w2_s", C.c_void_p),
                 ("add", C.c_void_p), ("ld_add", C.c_longlong), ("out", C.c_void_p), ("ld_out", C.c_longlong),
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+    _workspaces = _workspace_of = None                             # stream -> workspace allocated there (None: the caller's), the stream of the present one
 
 
 def library_path() -> str:
@@ -151,6 +152,12 @@ def _stream(stream=None):
     return C.c_void_p(s.cuda_stream)
 
 
+def _on(stream):
+    """What a call allocates comes from the pool of the stream that it runs on: memory of another stream's pool may still be in use there, and
+    would go back there while this call runs."""
+    return torch.cuda.stream(stream)
+
+
 def bf16_from_bits(bits: np.ndarray, device="cuda") -> torch.Tensor:
     """numpy uint16 bf16 patterns -> torch.bfloat16 tensor on the device."""
     return torch.from_numpy(np.ascontiguousarray(bits).view(np.int16)).to(device).view(torch.bfloat16)
@@ -203,15 +210,17 @@ def quantize_rows_fp4(x: torch.Tensor, stream=None):
     """realb_quantize_rows_fp4 on a bf16 [rows,K] tensor -> (q u8 [rows,K/2], s u8 K-step-tiled,
     ceil(rows/32)*32 * K/32 bytes; see scales_to_canonical)."""
     rows, K = x.shape
-    q = torch.empty((rows, K // 2), dtype=torch.uint8, device=x.device)
-    s = torch.zeros((-(-rows // 32) * 32, K // 32), dtype=torch.uint8, device=x.device)
+    with _on(stream):
+        q = torch.empty((rows, K // 2), dtype=torch.uint8, device=x.device)
+        s = torch.zeros((-(-rows // 32) * 32, K // 32), dtype=torch.uint8, device=x.device)
     _check(load_library().realb_quantize_rows_fp4(_p(x), rows, K, _p(q), _p(s), _stream(stream)))
     return q, s
 
 
 def amax_bf16(x: torch.Tensor, stream=None) -> torch.Tensor:
     """realb_amax_bf16: max |x| of a bf16 tensor (element count a multiple of 8) as a 1-element float tensor."""
-    out = torch.empty(1, dtype=torch.float32, device=x.device)
+    with _on(stream):
+        out = torch.empty(1, dtype=torch.float32, device=x.device)
     _check(load_library().realb_amax_bf16(_p(x), x.numel(), _p(out), _stream(stream)))
     return out
 
@@ -219,8 +228,9 @@ def amax_bf16(x: torch.Tensor, stream=None) -> torch.Tensor:
 def quantize_rows_nvfp4(x: torch.Tensor, global_scale: float, stream=None):
     """realb_quantize_rows_nvfp4 on a bf16 [rows,K] tensor -> (q u8 [rows,K/2], s u8 [rows,K/16] E4M3 bytes)."""
     rows, K = x.shape
-    q = torch.empty((rows, K // 2), dtype=torch.uint8, device=x.device)
-    s = torch.empty((rows, K // 16), dtype=torch.uint8, device=x.device)
+    with _on(stream):
+        q = torch.empty((rows, K // 2), dtype=torch.uint8, device=x.device)
+        s = torch.empty((rows, K // 16), dtype=torch.uint8, device=x.device)
     _check(load_library().realb_quantize_rows_nvfp4(_p(x), rows, K, C.c_float(global_scale), _p(q), _p(s), _stream(stream)))
     return q, s
 
@@ -317,7 +327,9 @@ class Fp8Weight:
 
 def quantize_rows_fp8(x: torch.Tensor, out: "Fp8Rows | None" = None, stream=None) -> Fp8Rows:
     """realb_quantize_rows_fp8 on a bf16 [rows, K] tensor with dense rows of any pitch."""
-    out = Fp8Rows.empty(*x.shape, device=x.device) if out is None else out
+    if out is None:
+        with _on(stream):
+            out = Fp8Rows.empty(*x.shape, device=x.device)
     ld = _rows(x, "x", (out.rows, out.K), _BF16_ONLY)
     _same_device(x, out.q, out.s)
     _check(load_library().realb_quantize_rows_fp8(x.data_ptr(), ld, out.rows, out.K, out.q.data_ptr(), out.ld, out.s.data_ptr(), out.ld_s, _stream(stream)))
@@ -326,7 +338,9 @@ def quantize_rows_fp8(x: torch.Tensor, out: "Fp8Rows | None" = None, stream=None
 
 def quantize_blocks_fp8(w: torch.Tensor, out: "Fp8Weight | None" = None, stream=None) -> Fp8Weight:
     """realb_quantize_blocks_fp8 on a dense bf16 [.., N, K] tensor."""
-    out = Fp8Weight.empty(*w.shape, device=w.device) if out is None else out
+    if out is None:
+        with _on(stream):
+            out = Fp8Weight.empty(*w.shape, device=w.device)
     if w.dtype is not torch.bfloat16 or not w.is_contiguous() or w.shape != out.q.shape:
         raise RealbError(f"w must be dense bfloat16 {tuple(out.q.shape)}")
     _same_device(w, out.q, out.s)
@@ -400,13 +414,12 @@ def linear_fp8(io: LinearIO, stream=None):
 
 def make_ffn_io(x: Fp8Rows, w13: Fp8Weight, w2: Fp8Weight, out: torch.Tensor, add=None, workspace=None, f32_sums: bool = False) -> FfnIO:
     """Arguments of gated_ffn_fp8: w13 [2I, H], w2 [H, I], out bf16 [rows, H], add bf16 (may be out).  workspace: dense u8 of at least
-    realb_gated_ffn_workspace_bytes(rows, I); allocated here if not given.  f32_sums: FP32 sums in both products, whatever the number of
+    realb_gated_ffn_workspace_bytes(rows, I), for one call at a time; if not given, allocated here for the current stream and by the first call on
+    any other stream for that one, and kept with the arguments.  f32_sums: FP32 sums in both products, whatever the number of
     rows (up to 64 they always are); without it more rows take the 8-bit instruction, faster and 0.0018 to 0.0026 off the formula, not 0.0017."""
     H, I = x.K, w2.K
     _require(tuple(w13.q.shape) == (2 * I, H) and tuple(w2.q.shape) == (H, I), f"weights {tuple(w13.q.shape)} and {tuple(w2.q.shape)} do not go with rows of {H}")
-    need = int(load_library().realb_gated_ffn_workspace_bytes(x.rows, I))
-    workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=out.device) if workspace is None else workspace
-    _require(workspace.dtype == torch.uint8 and workspace.is_contiguous(), "workspace must be dense uint8")
+    _require(workspace is None or (workspace.dtype == torch.uint8 and workspace.is_contiguous()), "workspace must be dense uint8")
     io = FfnIO()
     io.T, io.H, io.I, io.sums = x.rows, H, I, int(bool(f32_sums))
     io.x_q, io.ld_x, io.x_s, io.ld_xs = x.q.data_ptr(), x.ld, x.s.data_ptr(), x.ld_s
@@ -414,14 +427,31 @@ def make_ffn_io(x: Fp8Rows, w13: Fp8Weight, w2: Fp8Weight, out: torch.Tensor, ad
     if add is not None:
         io.add, io.ld_add = add.data_ptr(), _rows(add, "add", (x.rows, H), (torch.bfloat16,))
     io.out, io.ld_out = out.data_ptr(), _rows(out, "out", (x.rows, H), (torch.bfloat16,))
-    io.workspace, io.workspace_bytes = workspace.data_ptr(), workspace.numel()
     _same_device(x.q, x.s, w13.q, w13.s, w2.q, w2.s, out, add, workspace)
     io._keep = (x, w13, w2, out, add, workspace)
+    if workspace is None:
+        io._workspaces = {}
+        _own_workspace(io, None, _raw_stream(None))
+    else:
+        io.workspace, io.workspace_bytes = workspace.data_ptr(), workspace.numel()
     return io
 
 
+def _own_workspace(io: FfnIO, stream, raw: int):
+    """The workspace of the stream, allocated at its first call."""
+    own = io._workspaces.get(raw)
+    if own is None:
+        need = int((_LIB or load_library()).realb_gated_ffn_workspace_bytes(io.T, io.I))
+        with _on(stream):
+            own = io._workspaces[raw] = torch.empty(max(need, 16), dtype=torch.uint8, device=io._keep[0].q.device)
+    io.workspace, io.workspace_bytes, io._workspace_of = own.data_ptr(), own.numel(), raw
+
+
 def gated_ffn_fp8(io: FfnIO, stream=None):
-    rc = (_LIB or load_library()).realb_gated_ffn_fp8(C.byref(io), _raw_stream(stream))
+    raw = _raw_stream(stream)
+    if io._workspaces is not None and io._workspace_of != raw:
+        _own_workspace(io, stream, raw)
+    rc = (_LIB or load_library()).realb_gated_ffn_fp8(C.byref(io), raw)
     if rc:
         _check(rc)
 

@@ -45,3 +45,103 @@ def test_a_call_refuses_only_what_it_cannot_use():
         for room, why in ((need - 1, b"workspace"), (need, b"rows of out"), (lib.realb_gated_ffn_workspace_bytes(65, 128), b"rows of out")):
             assert lib.realb_gated_ffn_fp8(C.byref(_ffn_io(T=T, ld_xs=T, workspace_bytes=room, ld_out=1)), None) == -1
             assert why in lib.realb_last_error(), (T, room, lib.realb_last_error())
+
+
+# ---- streams: the binding on CPU tensors, with stand-ins for streams, their memory pools and the library
+class _Stream:
+    def __init__(self, number):
+        self.cuda_stream, self.device_index = number, 0
+
+
+@pytest.fixture
+def pools(monkeypatch):
+    """current: the stream whose pool serves an allocation; pool_of: address -> stream; calls: (operator, stream, workspace)."""
+    class World:
+        current, pool_of, calls, kept = 1, {}, [], []
+        needs = R.load_library().realb_gated_ffn_workspace_bytes
+
+    class On:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            self.before = World.current
+            World.current = World.current if self.stream is None else self.stream.cuda_stream
+
+        def __exit__(self, *_):
+            World.current = self.before
+
+    def recorded(make):
+        def alloc(*a, **k):
+            t = make(*a, **k)
+            World.pool_of[t.data_ptr()] = World.current
+            World.kept.append(t)
+            return t
+        return alloc
+
+    class Library:
+        realb_gated_ffn_workspace_bytes = staticmethod(World.needs)
+
+        def __getattr__(self, name):
+            def call(*a):
+                at = a[0]._obj.workspace if name == "realb_gated_ffn_fp8" else None
+                stream = a[-1].value if isinstance(a[-1], C.c_void_p) else a[-1]
+                World.calls.append((name, stream, at, a))
+                return 0
+            return call
+
+    monkeypatch.setattr(B, "_LIB", Library())
+    monkeypatch.setattr(B, "_same_device", lambda first, *others: 0)
+    monkeypatch.setattr(torch.cuda, "stream", On)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: _Stream(World.current))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch, "empty", recorded(torch.empty))
+    monkeypatch.setattr(torch, "zeros", recorded(torch.zeros))
+    return World
+
+
+def _u8(*s):
+    return torch.ones(s, dtype=torch.uint8)
+
+
+def _f32(*s):
+    return torch.ones(s, dtype=torch.float32)
+
+
+def _ffn_args(T=100, H=128, I=128):
+    return (R.Fp8Rows(_u8(T, H), _f32(1, T)), R.Fp8Weight(_u8(2 * I, H), _f32(2, 1)), R.Fp8Weight(_u8(H, I), _f32(1, 1)),
+            torch.ones((T, H), dtype=torch.bfloat16))
+
+
+def test_a_workspace_comes_from_the_pool_of_the_stream_that_uses_it(pools):
+    """Memory of another stream's pool may be in use there, and goes back there while the call still runs."""
+    io = R.make_ffn_io(*_ffn_args())
+    for stream in (None, _Stream(7), _Stream(8), _Stream(7), None):
+        R.gated_ffn_fp8(io, stream=stream)
+    used = [(stream, at) for _, stream, at, _ in pools.calls]
+    assert [s for s, _ in used] == [1, 7, 8, 7, 1]
+    assert all(pools.pool_of[at] == s for s, at in used)
+    assert used[1] == used[3] and used[0] == used[4]     # one workspace a stream, kept with the argument block
+    with torch.cuda.stream(_Stream(9)):                  # made under a stream
+        io = R.make_ffn_io(*_ffn_args())
+        R.gated_ffn_fp8(io)
+    R.gated_ffn_fp8(io)
+    assert [(s, pools.pool_of[at]) for _, s, at, _ in pools.calls[-2:]] == [(9, 9), (1, 1)]
+
+
+def test_a_workspace_of_the_callers_stays_in_use_on_every_stream(pools):
+    work = _u8(100 * 128 + 400 + 64 * 128 * 4)
+    io = R.make_ffn_io(*_ffn_args(), workspace=work)
+    for stream in (None, _Stream(7)):
+        R.gated_ffn_fp8(io, stream=stream)
+    assert [at for _, _, at, _ in pools.calls] == [work.data_ptr()] * 2
+
+
+@pytest.mark.parametrize("stream,pool", [(None, 1), (_Stream(7), 7)])
+def test_encoders_allocate_where_they_run(pools, stream, pool):
+    x = torch.ones((32, 128), dtype=torch.bfloat16)
+    rows, w = R.quantize_rows_fp8(x, stream=stream), R.quantize_blocks_fp8(x, stream=stream)
+    fp4, nv = R.quantize_rows_fp4(x, stream=stream), R.quantize_rows_nvfp4(x, 1.0, stream=stream)
+    for t in (rows.q, rows.s, w.q, w.s, *fp4, *nv, R.amax_bf16(x, stream=stream)):
+        assert pools.pool_of[t.data_ptr()] == pool
+    assert [s for _, s, _, _ in pools.calls] == [pool] * 5
