@@ -54,6 +54,7 @@ class NormIO(C.Structure):
                 ("gate", C.c_void_p), ("ld_gate", C.c_longlong), ("gate_step", C.c_int),
                 ("res_out", C.c_void_p), ("ld_res_out", C.c_longlong), ("pre_w", C.c_void_p), ("out", C.c_void_p), ("ld_out", C.c_longlong),
                 ("out_q", C.c_void_p), ("ld_q", C.c_longlong), ("out_s", C.c_void_p), ("ld_s", C.c_longlong)]
+    _gpu = None                                          # the tensors' GPU
 
 
 class LinearIO(C.Structure):
@@ -61,6 +62,7 @@ class LinearIO(C.Structure):
                 ("x_q", C.c_void_p), ("ld_x", C.c_longlong), ("x_s", C.c_void_p), ("ld_xs", C.c_longlong),
                 ("w_q", C.c_void_p), ("w_s", C.c_void_p), ("bias", C.c_void_p), ("add", C.c_void_p), ("ld_add", C.c_longlong),
                 ("out_type", C.c_int), ("out", C.c_void_p), ("ld_out", C.c_longlong)]
+    _gpu = None
 
 
 class FfnIO(C.Structure):
@@ -69,7 +71,8 @@ class FfnIO(C.Structure):
                 ("w13_q", C.c_void_p), ("w13_s", C.c_void_p), ("w2_q", C.c_void_p), ("w2_s", C.c_void_p),
                 ("add", C.c_void_p), ("ld_add", C.c_longlong), ("out", C.c_void_p), ("ld_out", C.c_longlong),
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
-    _workspaces = _workspace_of = None                             # stream -> workspace allocated there (None: the caller's), the stream of the present one
+    _gpu = None
+    _workspaces = _workspace_of = None                   # stream -> workspace allocated there (None: the caller's), the stream of the present one
 
 
 def library_path() -> str:
@@ -277,12 +280,22 @@ def _vector(t, name: str, n: int):
     return t.data_ptr()
 
 
-def _same_device(first, *others):
+def _same_device(first, *others) -> int:
     gpu = first.get_device()
     for t in others:
         if t is not None and t.get_device() != gpu:
             gpu = -1
     _require(gpu >= 0, "tensors are not on one GPU")
+    return gpu
+
+
+def _raw_stream(stream, gpu):
+    """As _stream, a plain number: these calls are short enough for the difference to show.  gpu: the tensors' one (None: arguments that were not
+    made here).  Kernels are launched on the current GPU, so all three have to agree."""
+    s = torch.cuda.current_stream() if stream is None else stream
+    if gpu is not None and (s.device_index != gpu or (stream is not None and torch.cuda.current_device() != gpu)):
+        raise RealbError(f"the tensors are on GPU {gpu}, the stream on {s.device_index}, the current one is {torch.cuda.current_device()}")
+    return s.cuda_stream
 
 
 class Fp8Rows:
@@ -331,8 +344,8 @@ def quantize_rows_fp8(x: torch.Tensor, out: "Fp8Rows | None" = None, stream=None
         with _on(stream):
             out = Fp8Rows.empty(*x.shape, device=x.device)
     ld = _rows(x, "x", (out.rows, out.K), _BF16_ONLY)
-    _same_device(x, out.q, out.s)
-    _check(load_library().realb_quantize_rows_fp8(x.data_ptr(), ld, out.rows, out.K, out.q.data_ptr(), out.ld, out.s.data_ptr(), out.ld_s, _stream(stream)))
+    raw = _raw_stream(stream, _same_device(x, out.q, out.s))
+    _check(load_library().realb_quantize_rows_fp8(x.data_ptr(), ld, out.rows, out.K, out.q.data_ptr(), out.ld, out.s.data_ptr(), out.ld_s, raw))
     return out
 
 
@@ -343,9 +356,9 @@ def quantize_blocks_fp8(w: torch.Tensor, out: "Fp8Weight | None" = None, stream=
             out = Fp8Weight.empty(*w.shape, device=w.device)
     if w.dtype is not torch.bfloat16 or not w.is_contiguous() or w.shape != out.q.shape:
         raise RealbError(f"w must be dense bfloat16 {tuple(out.q.shape)}")
-    _same_device(w, out.q, out.s)
+    raw = _raw_stream(stream, _same_device(w, out.q, out.s))
     mats = w.numel() // max(1, out.N * out.K) if w.dim() > 2 else 1
-    _check(load_library().realb_quantize_blocks_fp8(w.data_ptr(), mats, out.N, out.K, out.q.data_ptr(), out.s.data_ptr(), _stream(stream)))
+    _check(load_library().realb_quantize_blocks_fp8(w.data_ptr(), mats, out.N, out.K, out.q.data_ptr(), out.s.data_ptr(), raw))
     return out
 
 
@@ -374,18 +387,13 @@ def make_norm_io(res, y=None, res_out=None, post_weight=None, gate=None, scale: 
     if out_fp8 is not None:
         _require((out_fp8.rows, out_fp8.K) == (T, H), f"out_fp8 is [{out_fp8.rows}, {out_fp8.K}], expected [{T}, {H}]")
         io.out_q, io.ld_q, io.out_s, io.ld_s = out_fp8.q.data_ptr(), out_fp8.ld, out_fp8.s.data_ptr(), out_fp8.ld_s
-    _same_device(res, y, post_weight, pre_weight, gate, res_out, out, *((out_fp8.q, out_fp8.s) if out_fp8 else ()))
+    io._gpu = _same_device(res, y, post_weight, pre_weight, gate, res_out, out, *((out_fp8.q, out_fp8.s) if out_fp8 else ()))
     io._keep = (res, y, res_out, post_weight, gate, pre_weight, out, out_fp8)
     return io
 
 
-def _raw_stream(stream):
-    """As _stream, a plain number: these calls are short enough for the difference to show."""
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
-
-
 def residual_norm(io: NormIO, stream=None):
-    rc = (_LIB or load_library()).realb_residual_norm(C.byref(io), _raw_stream(stream))
+    rc = (_LIB or load_library()).realb_residual_norm(C.byref(io), _raw_stream(stream, io._gpu))
     if rc:
         _check(rc)
 
@@ -401,13 +409,13 @@ def make_linear_io(x: Fp8Rows, w: Fp8Weight, out: torch.Tensor, bias=None, add=N
         io.add, io.ld_add = add.data_ptr(), _rows(add, "add", (x.rows, w.N), (out.dtype,))
     io.ld_out = _rows(out, "out", (x.rows, w.N), _TYPES)
     io.out, io.out_type = out.data_ptr(), _TYPES[out.dtype]
-    _same_device(x.q, x.s, w.q, w.s, out, bias, add)
+    io._gpu = _same_device(x.q, x.s, w.q, w.s, out, bias, add)
     io._keep = (x, w, out, bias, add)
     return io
 
 
 def linear_fp8(io: LinearIO, stream=None):
-    rc = (_LIB or load_library()).realb_linear_fp8(C.byref(io), _raw_stream(stream))
+    rc = (_LIB or load_library()).realb_linear_fp8(C.byref(io), _raw_stream(stream, io._gpu))
     if rc:
         _check(rc)
 
@@ -427,11 +435,11 @@ def make_ffn_io(x: Fp8Rows, w13: Fp8Weight, w2: Fp8Weight, out: torch.Tensor, ad
     if add is not None:
         io.add, io.ld_add = add.data_ptr(), _rows(add, "add", (x.rows, H), (torch.bfloat16,))
     io.out, io.ld_out = out.data_ptr(), _rows(out, "out", (x.rows, H), (torch.bfloat16,))
-    _same_device(x.q, x.s, w13.q, w13.s, w2.q, w2.s, out, add, workspace)
+    io._gpu = _same_device(x.q, x.s, w13.q, w13.s, w2.q, w2.s, out, add, workspace)
     io._keep = (x, w13, w2, out, add, workspace)
     if workspace is None:
         io._workspaces = {}
-        _own_workspace(io, None, _raw_stream(None))
+        _own_workspace(io, None, _raw_stream(None, None))
     else:
         io.workspace, io.workspace_bytes = workspace.data_ptr(), workspace.numel()
     return io
@@ -448,7 +456,7 @@ def _own_workspace(io: FfnIO, stream, raw: int):
 
 
 def gated_ffn_fp8(io: FfnIO, stream=None):
-    raw = _raw_stream(stream)
+    raw = _raw_stream(stream, io._gpu)
     if io._workspaces is not None and io._workspace_of != raw:
         _own_workspace(io, stream, raw)
     rc = (_LIB or load_library()).realb_gated_ffn_fp8(C.byref(io), raw)

@@ -145,3 +145,37 @@ def test_encoders_allocate_where_they_run(pools, stream, pool):
     for t in (rows.q, rows.s, w.q, w.s, *fp4, *nv, R.amax_bf16(x, stream=stream)):
         assert pools.pool_of[t.data_ptr()] == pool
     assert [s for _, s, _, _ in pools.calls] == [pool] * 5
+
+
+def _calls_on(stream):
+    """Every call of the operators around the layer on `stream`, as functions."""
+    bf = lambda *s: torch.ones(s, dtype=torch.bfloat16)  # noqa: E731
+    x, w13, w2, out = _ffn_args()
+    norm = R.make_norm_io(bf(4, 128), res_out=bf(4, 128))
+    linear, ffn = R.make_linear_io(x, w2, bf(100, 128)), R.make_ffn_io(x, w13, w2, out, workspace=_u8(1 << 17))
+    return [lambda: R.residual_norm(norm, stream=stream), lambda: R.linear_fp8(linear, stream=stream), lambda: R.gated_ffn_fp8(ffn, stream=stream),
+            lambda: R.quantize_rows_fp8(bf(100, 128), out=x, stream=stream), lambda: R.quantize_blocks_fp8(bf(128, 128), out=w2, stream=stream)]
+
+
+@pytest.mark.parametrize("tensors,current,stream", [(1, 0, None), (1, 1, 0), (1, 0, 1), (0, 1, None), (0, 0, 1)])
+def test_tensors_of_another_gpu_than_the_calls_are_refused(pools, monkeypatch, tensors, current, stream):
+    """The kernels are launched on the current GPU: another GPU's stream or tensors would be a launch error, or addresses it cannot reach."""
+    monkeypatch.setattr(B, "_same_device", lambda first, *others: tensors)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
+
+    def on(gpu):
+        s = _Stream(5)
+        s.device_index = gpu
+        return s
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: on(current))
+    for call in _calls_on(None if stream is None else on(stream)):
+        with pytest.raises(R.RealbError, match="GPU"):
+            call()
+    assert not pools.calls
+
+
+def test_calls_on_the_tensors_gpu_go_through(pools):
+    for stream in (None, _Stream(7)):
+        for call in _calls_on(stream):
+            call()
+    assert len(pools.calls) == 10
