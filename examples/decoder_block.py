@@ -4,38 +4,53 @@
     stream  += projection;  x = norm(stream)                              residual_norm, x in BF16 and in E4M3
     logits  = x . router                                                  E4M3 product with F32 output
     routed  = this rank's experts                                         layer_forward (BF16 or FP4, by the policy)
+    routed  = the sum of all ranks' routed                                all-reduce
     y       = shared expert(x) + routed                                   gated_ffn_fp8
     stream  += scale * y;  next input = norm(stream)                      residual_norm
 
-python examples/decoder_block.py [tokens ...]  prints the time of a pass for each number of tokens (Kimi-VL-shaped layer)."""
+Tokens, stream and dense weights are the same on every rank, the experts are split over the ranks.  The router is an E4M3 product here to show
+one with F32 output; it decides the routing in 8 bits, where models keep that matrix in BF16 or F32.
+
+python examples/decoder_block.py [tokens ...]  prints the time of a pass for each number of tokens (Kimi-VL-shaped layer), all experts on one GPU;
+python -m torch.distributed.run --nproc-per-node N --master-addr 127.0.0.1 examples/decoder_block.py [tokens ...]  splits them over N."""
 from __future__ import annotations
 
 import os
 import sys
 
 import torch
+import torch.distributed as dist
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2604_19503_amd as R  # noqa: E402
 from paper_2604_19503_amd.binding import default_config  # noqa: E402
 
 
+def sum_over_ranks(partial: torch.Tensor):
+    """The ranks' partial outputs of the layer, summed in place on each of them (BF16, as they are)."""
+    dist.all_reduce(partial)
+
+
 class DecoderBlockHalf:
-    """Weights, buffers and calls of one layer for T tokens.  The stream is updated in place by run()."""
+    """Weights, buffers and calls of one layer for T tokens on one of D ranks.  The stream is updated in place by run().  sum_ranks adds the other
+    ranks' outputs to this one's partial output, in place on the current stream; without it a rank of several gives only its own experts' share."""
 
     def __init__(self, T: int, E: int = 64, k: int = 6, D: int = 8, H: int = 2048, I: int = 1408, I_shared: int = 1408, rank: int = 0,
-                 force: int = R.FORCE_NONE, scale: float = 1.0, seed: int = 0):
-        gen = torch.Generator(device="cuda")
-        gen.manual_seed(seed)
+                 force: int = R.FORCE_NONE, scale: float = 1.0, seed: int = 0, sum_ranks=None):
+        gen, of_rank = torch.Generator(device="cuda"), torch.Generator(device="cuda")
+        gen.manual_seed(seed)                            # what all ranks have alike
+        of_rank.manual_seed(1000 * (seed + 1) + rank)    # this rank's experts
 
-        def bf16(*shape, std=0.02):
+        def bf16(*shape, std=0.02, gen=gen):
             return torch.randn(shape, generator=gen, device="cuda").mul_(std).to(torch.bfloat16)
+
+        self.sum_ranks = sum_ranks
 
         self.cfg = default_config(T, E, k, D, H, I)
         self.ctx = R.Context(self.cfg)
         nl = E // D
         # weights; what is dense is encoded once
-        self.w13, self.w2 = bf16(nl, 2 * I, H), bf16(nl, H, I)
+        self.w13, self.w2 = bf16(nl, 2 * I, H, gen=of_rank), bf16(nl, H, I, gen=of_rank)
         self.w_o, self.w_router, self.w_shared13, self.w_shared2 = bf16(H, H), bf16(E, H, std=0.5), bf16(2 * I_shared, H), bf16(H, I_shared)
         o_proj, router, shared13, shared2 = (R.quantize_blocks_fp8(w) for w in (self.w_o, self.w_router, self.w_shared13, self.w_shared2))
         self.norm_w, self.next_norm_w = (1.0 + bf16(H, std=0.1).float()).to(torch.bfloat16), (1.0 + bf16(H, std=0.1).float()).to(torch.bfloat16)
@@ -61,14 +76,20 @@ class DecoderBlockHalf:
         R.residual_norm(self.pre_norm)
         R.linear_fp8(self.route)
         precision = self.ctx.layer_forward(self.experts)
+        if self.sum_ranks is not None:
+            self.sum_ranks(self.buf.out)
         R.gated_ffn_fp8(self.shared)
         R.residual_norm(self.post_norm)
         return precision
 
 
 def main():
+    ranks, rank = int(os.environ.get("WORLD_SIZE", 1)), int(os.environ.get("RANK", 0))
+    if ranks > 1:
+        torch.cuda.set_device(int(os.environ["LOCAL_RANK"]))
+        dist.init_process_group("nccl")
     for T in [int(a) for a in sys.argv[1:]] or [1, 24, 1000, 16384]:
-        half = DecoderBlockHalf(T)
+        half = DecoderBlockHalf(T, D=ranks, rank=rank, sum_ranks=sum_over_ranks if ranks > 1 else None)
         precision = half.run()
         torch.cuda.synchronize()
         begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
@@ -78,7 +99,10 @@ def main():
             half.run()
         end.record()
         torch.cuda.synchronize()
-        print(f"{T} tokens: {begin.elapsed_time(end) * 1e3 / n:.1f} us a pass, experts in {'FP4' if precision else 'BF16'}", flush=True)
+        if rank == 0:
+            print(f"{T} tokens: {begin.elapsed_time(end) * 1e3 / n:.1f} us a pass, experts in {'FP4' if precision else 'BF16'}", flush=True)
+    if ranks > 1:
+        dist.destroy_process_group()
 
 
 if __name__ == "__main__":
