@@ -95,6 +95,7 @@ __device__ __forceinline__ void fp8_store_tile(const Fp8Gemm& p, v4f_t (&acc)[RT
 #pragma unroll
             for (int e = 0; e < 8; ++e) {                   // h takes the gate's place
                 const float gate = acc[i][e >> 2][e & 3], up = acc[i][2 + (e >> 2)][e & 3];
+                // (reciprocal and exponential to a few ulp, some 1e-7 of h, where half a code's step is 1/16 of it; a division is ten instructions)
                 const float h = gate * __builtin_amdgcn_rcpf(1.0f + __expf(-gate)) * up;
                 acc[i][e >> 2][e & 3] = h;
                 m = fmaxf(m, fabsf(h));
@@ -208,12 +209,14 @@ __device__ __forceinline__ void fp8_store_tile(const Fp8Gemm& p, v4f_t (&acc)[RT
 
 // Small tiles, for products that have too few large ones to fill the chip: 16*RT*WM activation rows x 16*CT*WN weight rows, WM x WN waves of
 // 16*RT x 16*CT.  A K-step is 128 bytes of every row, brought to LDS without passing through registers (8 rows per instruction; the 16-byte
-// parts of row R sit XOR-swizzled by (R >> 1) & 7, which keeps the fragment reads free of bank conflicts); NS stages, NS - 1 steps
+// parts of row R sit XOR-swizzled by (R >> 1) & 7, which keeps the fragment reads free of bank conflicts); NS stages filled NS - 1 steps
 // ahead, one barrier per step.  K is summed in order, as in the large tiles, so the bits of a row do not depend on which tiles it is in.
-// Bound by what a wave does one after the other in a step (transfers, fragments, MFMAs, multiply-adds: 0.4 us for 64 columns per wave,
-// however deep the pipeline and with one or two K blocks per step), so few tiles get more waves of fewer columns: 65 rows, N = K = 2048, 64 x 64
-// tiles, 4 waves of 16 x 64 8.7 us, 8 waves of 16 x 32 7.2 us; 2000 rows x 1408 x 4096, 128 x 128 tiles, 8 waves 29.6, 16 waves 24.0 us;
-// gate/up tiles of 128 x 256, 8 waves of 64 x 64 or 16 of 32 x 64: the feed-forward block of 3001 rows, H 2048, I 768 33.0 / 32.2 us.
+// Bound by the transfers' latency, once a step: the wait at the step's barrier counts, but the loop may load weight scales (every 64th
+// step), so the compiler waits for all vector memory in front of the lane reads of them in each step, and with it for the transfers that
+// the step before sent.  That makes 0.35 to 0.4 us a step whatever NS is (two K blocks per step, six and eight stages changed nothing; they were
+// measured with this wait and say nothing about a pipeline without it), and few tiles get more waves of fewer columns: 65 rows, N = K = 2048, 64 x 64
+// tiles, 4 waves of 16 x 64 8.7 us, 8 waves of 16 x 32 7.4 us; 2000 rows x 1408 x 4096, 128 x 128 tiles, 8 waves 29.6, 16 waves 25 us;
+// gate/up tiles of 128 x 256, 8 waves of 64 x 64 or 16 of 32 x 64: the feed-forward block of 3001 rows, H 2048, I 768 33.0 / 32.3 us.
 template <int RT, int WM, int WN, int NS, int CT>
 struct SmallGeo {
     static constexpr int TA = 16 * RT * WM, TW = 16 * CT * WN, WAVES = WM * WN;
@@ -274,7 +277,8 @@ __global__ void __launch_bounds__(64 * WM * WN) fp8_tile_kernel(const Fp8Gemm p)
     const int nb = GATEUP ? n0 >> 7 : min((n0 + wn * 16 * CT) >> 7, (p.N - 1) >> 7);
     const float* ws0 = p.ws + (long long)nb * p.KB;
     const float* ws1 = GATEUP ? ws0 + (long long)(p.N >> 7) * p.KB : ws0;
-    // the weights' scales: lane l holds those of K block l, 64 + l, ..  (scalar loads would be waited for together with the fragments)
+    // the weights' scales: lane l holds those of K block l, 64 + l, ..  (scalar loads in each step, waited for together with the fragments,
+    // were slower: 65 rows 10.4 -> 8.4 us)
     float wsv[2] = {0.f, 0.f};
     auto load_scales = [&](int kb) __attribute__((always_inline)) {
         wsv[0] = ws0[min(kb + lane, p.KB - 1)];
@@ -328,8 +332,9 @@ __global__ void __launch_bounds__(64 * WM * WN) fp8_tile_kernel(const Fp8Gemm p)
 // column tiles), whose multiply-adds onto the accumulators run beside the MFMAs behind them:
 //   section 0: fragments of the weights and of rows 0..63; transfers of the next step's rows
 //   section 1: of rows 64..127; transfers of the weights of the step after; the next step has landed
-// Bound by the matrix cores and the power limit: 8192^3 428 us (2570 TFLOP/s; 366 without transfers, 360 with operands of zeros), 32768 x 4096 x 2048
-// 230 us (2390), where the epilogue's 3.6 us a tile count.  Four turns a step instead of two took 304 us there.
+// Bound by power and by the change of turns: the matrix cores are busy in 52 % of the cycles, at 2.0 GHz; 8192^3 takes 428 to 450 us (2440 to 2570
+// TFLOP/s; 366 without transfers, 360 with operands of zeros), 32768 x 4096 x 2048 236 to 260 (2110 to 2330; 270 when launched without a pause
+// for milliseconds), where the epilogue's 3.6 us a tile count.  Four turns a step instead of two took 304 us there (two: 255 at that time).
 struct BigGeo {
     static constexpr int TA = 256, TW = 256;
     static constexpr int STAGE = (TA + TW) * 128;
@@ -339,7 +344,8 @@ struct BigGeo {
     static constexpr int LDS = AMAX + 4 * TA * 4;
 };
 constexpr long long kBigMaxPitch = 1 << 23;               // 256 rows of this pitch are within 32-bit offsets
-constexpr int kBigMaxBlocks = 64;                          // K blocks whose weight scales one transfer of a wave holds
+// K blocks whose weight scales one transfer of a wave holds.  Above, K > 8192, small tiles: 8192 x 8192 x 8192 465 us, 8192 x 8192 x 8208 823.
+constexpr int kBigMaxBlocks = 64;
 
 template <bool GATEUP, bool RAGGED, bool NT>
 __global__ void __launch_bounds__(512, 1) fp8_big_kernel(const Fp8Gemm p) {
@@ -546,13 +552,14 @@ __global__ void __launch_bounds__(512, 1) fp8_big_kernel(const Fp8Gemm p) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no transfer may still be writing this block's LDS when it ends
 }
 
-// Few rows (decode steps): the weights' bytes are what takes the time, so they go from memory straight to registers, all of a wave's
-// at once, and the waves of a block share the K blocks of 16 weight rows; their sums meet in LDS, in the order of the waves.  The
+// Few rows (decode steps): the weights' bytes are what takes the time, so they go from memory straight to registers, AHEAD K blocks of a
+// wave's behind one another (between two of them the wave waits for the weights' scale, a scalar load; down: one K block at a time), and
+// the waves of a block share the K blocks of 16 weight rows; their sums meet in LDS, in the order of the waves.  The
 // rows come from the caches: a block reads all of them.  Sums are FP32 here (see above).  Gate/up: 8 gate and 8 up rows, so that I = 1408
 // makes 176 blocks.  h of the feed-forward block: gate/up leaves it in FP32, and the down product's waves encode the blocks of it that
 // they multiply: an E4M3 block spans 128 columns, which would leave a block per 128 columns of h, 11, to read the weights.
-// One row: 8192 x 8192 13.1 us (5.1 TB/s), 2048 x 2048 3.1 us (launch and one memory latency); 24 rows 4.4 us; the feed-forward block of 24
-// rows, H 2048, I 1408 10.5 us.  8 waves per block; 4 and 16 were slower, so were non-temporal loads.
+// One row: 8192 x 8192 13.1 to 13.8 us (5.1 TB/s), 2048 x 2048 3.1 us (launch, the scales' latencies and the weights'); 24 rows 4.8 us; the
+// feed-forward block of 24 rows, H 2048, I 1408 10.7 us.  8 waves per block; 4 and 16 were slower, so were non-temporal loads.
 enum FewKind { kFewLinear, kFewLinearF32, kFewGateUp, kFewDown };
 
 // Where h of (row m, column k) of M rows is: column 64 a + 16 g + 4 q + r of a block of 128 sits with the other rows' and g's of the same
@@ -746,6 +753,11 @@ static int launch_fp8_big(Fp8Gemm p, hipStream_t s) {
     return REALB_OK;
 }
 
+// Up to here fp8_few_kernel, above tiles; products alone, us, few / tiles:   17 rows      32 rows      48 rows      64 rows
+//   2048 x 2048                                                           4.6 / 7.4    5.2 / 7.5    6.4 / 7.5    7.4 / 7.6
+//   2048 x 8192 (K)                                                      10.9 / 27.8  13.7 / 28.0  18.5 / 27.9  22.3 / 28.2
+//   8192 x 8192                                                          20.8 / 28.9  25.3 / 29.2  33.4 / 29.0  43.9 / 29.4
+// It is also where FP32 sums cost nothing, which the wide products of 33 to 64 rows pay for.
 constexpr int kFewRows = 64;
 template <int RT, FewKind KIND>
 static int launch_fp8_few_rows(const Fp8Gemm& p, hipStream_t s) {
@@ -774,8 +786,10 @@ static int launch_fp8_few(const Fp8Gemm& p, hipStream_t s) {
 //   64 x 256                      15       24
 //   128 x 256                     22       37
 //   256 x 256                     31
+// They are used for every K: between tiles the ratios hold roughly, but a launch weighs more where a round is short.
 // Where the last round of 256-row tiles would be short, the rows behind the whole rounds go to a second launch with smaller tiles, if that is
-// faster by more than a launch: 10 000 rows, K = N = 2048 51.2 -> 48.5 us; the feed-forward block of 6000 rows, H 2048, I 1408 82.7 -> 71.7 us.
+// faster by more than a launch.  One launch / two, us: 10 000 rows, N = 2048, K = 2048 54.6 / 51.1, 512 22.2 / 23.7, 128 14.4 / 16.3; 17 000 rows 85.5 / 79.6, 32.1 / 31.0,
+// 20.4 / 21.0; the feed-forward block of 6000 rows, I 1408, H = 2048 83.8 / 73.6, 1024 53.7 / 47.6, 128 25.5 / 23.4.
 enum Fp8Tile { kTile64, kTile128x64, kTile128One, kTile128, kTile256, kTileSplit };      // (Split: whole rounds of 256 and a second launch)
 struct Fp8Choice { Fp8Tile tile; int us; };
 
